@@ -459,15 +459,17 @@ statekv_status statekv_frame_attention_noalloc(const statekv_config* cfg, const 
  * position; sin, cos and the rotation are fp32 with one rounding to bf16.
  *   freq, axis  host arrays [num_pairs], read during the call: angular
  *               frequencies with |freq| < pi, axes in [0, num_axes)
- *   positions   int32 [num_axes][position_stride] (device)
+ *   positions   int32 [num_axes][position_stride] (device); a position_stride of 0
+ *               gives every axis the same row of num_tokens
  *   q, k        bf16 [num_tokens][heads][head_dim] (device), tokens q_stride /
  *               k_stride elements apart; a NULL q (or k) is skipped
  *   q_out, k_out  the same layout with their own strides; may equal q and k
  *               (in place, same stride) but not overlap them otherwise
  * INVALID_ARG for null or misaligned pointers (16 bytes; positions 4), a
- * stride below heads * head_dim or not a multiple of 8, num_axes outside
- * [1, 4], 2 num_pairs > head_dim; UNSUPPORTED for a head_dim that is not a
- * multiple of 8 or above 256.  num_tokens = 0 is a no-op. */
+ * stride below heads * head_dim or not a multiple of 8, a position_stride
+ * below num_tokens other than 0, num_axes outside [1, 4], 2 num_pairs > head_dim;
+ * UNSUPPORTED for a head_dim that is not a multiple of 8 or above 256.  num_tokens = 0
+ * is a no-op. */
 typedef struct {
     int32_t num_tokens, num_q_heads, num_kv_heads, head_dim;
     int32_t num_axes, num_pairs;

@@ -119,7 +119,9 @@ statekv_status statekv_mrope(const statekv_mrope_args* a, statekv_stream stream)
         p.axis[i] = static_cast<uint8_t>(a->axis[i]);
     }
     if (a->num_tokens == 0) return STATEKV_OK;
-    if (!a->positions || !aligned(a->positions, 4) || a->position_stride < a->num_tokens) return STATEKV_ERR_INVALID_ARG;
+    if (!a->positions || !aligned(a->positions, 4) || a->position_stride < 0 ||
+        (a->position_stride > 0 && a->position_stride < a->num_tokens))
+        return STATEKV_ERR_INVALID_ARG;
     const void* src[2] = {a->q, a->k};
     void* dst[2] = {a->q_out, a->k_out};
     const int64_t stride[2] = {a->q_stride, a->k_stride}, out_stride[2] = {a->q_out_stride, a->k_out_stride};

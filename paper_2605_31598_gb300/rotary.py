@@ -50,8 +50,9 @@ def _rows(x, tokens, heads, d, name):
 def mrope(q, k, positions, freq, axis, *, scale=1.0, adjacent=False, transpose=False, q_out=None,
           k_out=None, stream=None):
     """q and k (bf16 [tokens][heads][d], the rows of a token contiguous; either may
-    be None) turned at ``positions`` (int32 [axes][tokens], device); returns
-    (q_out, k_out), made here unless given (``q_out=q`` turns in place).
+    be None) turned at ``positions`` (int32 [axes][tokens], device; for text, whose
+    axes are equal, ``expand`` of one row will do); returns (q_out, k_out), made here
+    unless given (``q_out=q`` turns in place).
     ``freq``, ``axis``: CPU tensors as from ``mrope_frequencies``.  ``transpose``
     turns the other way: the gradient with respect to q and k.  Raises
     StateKVError on a bad argument."""
@@ -64,6 +65,9 @@ def mrope(q, k, positions, freq, axis, *, scale=1.0, adjacent=False, transpose=F
         raise ValueError("freq and axis: contiguous CPU tensors, fp64 and int32, one entry per pair")
     if positions.dtype != torch.int32 or width < tokens or (ps[1] != 1 and width > 1) or not positions.is_cuda:
         raise ValueError("positions: an int32 device tensor [axes][tokens]")
+    axis_stride = ps[0] if axes > 1 else width  # of one axis it has no meaning
+    if 0 < axis_stride < tokens:
+        raise ValueError("positions: axes that overlap (expanded from one, or at least a call's tokens apart)")
     hq = hk = q_ptr = k_ptr = qo_ptr = ko_ptr = qs = ks = qos = kos = 0
     if q is not None:
         hq = q.shape[1]
@@ -85,6 +89,6 @@ def mrope(q, k, positions, freq, axis, *, scale=1.0, adjacent=False, transpose=F
         k_ptr, ko_ptr = k.data_ptr(), k_out.data_ptr()
     call, pack = _call()
     check(call(pack(tokens, hq, hk, d, axes, pairs, adjacent, transpose, scale, freq.data_ptr(), axis.data_ptr(),
-                    positions.data_ptr(), max(ps[0], width), q_ptr, k_ptr, qo_ptr, ko_ptr, qs, ks, qos, kos),
+                    positions.data_ptr(), axis_stride, q_ptr, k_ptr, qo_ptr, ko_ptr, qs, ks, qos, kos),
                raw_stream(stream, positions)), "statekv_mrope")
     return q_out, k_out

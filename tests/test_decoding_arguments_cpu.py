@@ -1,0 +1,87 @@
+"""What the Python entry points of the decoding operators pass to the C calls, and
+what they refuse, with stand-ins for device tensors: nothing is enqueued."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_31598_gb300 import rotary
+
+
+class OnDevice:
+    """A CPU tensor that says it is on a CUDA device."""
+    is_cuda = True
+
+    def __init__(self, x, device=0):
+        self.x, self.index = x, device
+
+    def get_device(self):
+        return self.index
+
+    def __getattr__(self, name):
+        return getattr(self.x, name)
+
+
+class MropeCall:
+    """Stands for the C call of ``mrope``; keeps the fields of its arguments."""
+    NAMES = ("tokens", "hq", "hk", "d", "axes", "pairs", "adjacent", "transpose", "scale", "freq", "axis", "positions",
+             "position_stride", "q", "k", "q_out", "k_out", "q_stride", "k_stride", "q_out_stride", "k_out_stride")
+
+    def __init__(self, monkeypatch):
+        self.args = None
+        monkeypatch.setattr(rotary, "_call", lambda: (lambda args, stream: 0, self.pack))
+        monkeypatch.setattr(rotary, "raw_stream", lambda stream, x: 0)
+
+    def pack(self, *fields):
+        self.args = dict(zip(self.NAMES, fields))
+
+
+def turn(positions, tokens, **kw):
+    q = OnDevice(torch.zeros((tokens, 2, 64), dtype=torch.bfloat16))
+    freq, axis = rotary.mrope_frequencies((8, 12, 12)[:positions.shape[0]], 1e4)
+    return rotary.mrope(q, None, OnDevice(positions), freq, axis, q_out=q, **kw)
+
+
+@pytest.mark.parametrize("positions", [
+    torch.arange(40, 47, dtype=torch.int32).expand(3, 7),                       # text: one row for all axes
+    torch.tensor([9], dtype=torch.int32).expand(3, 1),
+    torch.arange(40, 52, dtype=torch.int32).expand(3, 12)[:, 2:9],              # a slice of such a row
+    torch.arange(60, dtype=torch.int32).view(3, 20)[:, 4:11],
+    torch.arange(60, dtype=torch.int32).view(3, 20)[1:2, 4:11],
+    torch.arange(9, dtype=torch.int32)[:, None][3:6],                           # a column
+    torch.arange(30, dtype=torch.int32).as_strided((3, 10), (8, 1)),            # wider than the call's tokens and its stride
+    torch.arange(7, dtype=torch.int32).as_strided((1, 7), (3, 1)),              # one axis: any stride
+], ids=str)
+def test_mrope_reads_the_positions_it_was_given(monkeypatch, positions):
+    """The kernel reads element axis * position_stride + token behind the pointer."""
+    call, tokens = MropeCall(monkeypatch), min(7, positions.shape[1])
+    turn(positions, tokens)
+    assert call.args["positions"] == positions.data_ptr() and call.args["axes"] == positions.shape[0]
+    held = np.frombuffer(bytes(positions.untyped_storage()), np.int32)[positions.storage_offset():]
+    at = np.arange(positions.shape[0])[:, None] * call.args["position_stride"] + np.arange(tokens)
+    assert at.max() < len(held)
+    assert np.array_equal(held[at], positions[:, :tokens].numpy())
+
+
+@pytest.mark.parametrize("positions", [
+    torch.arange(9, dtype=torch.int32).as_strided((3, 7), (1, 1)),   # overlapping windows
+    torch.arange(21, dtype=torch.int32).view(7, 3).T,                # a token's positions side by side
+    torch.arange(18, dtype=torch.int32).view(3, 6),                  # fewer than the tokens
+    torch.arange(21).view(3, 7),
+], ids=["overlapping", "transposed", "few", "int64"])
+def test_mrope_refuses_positions_it_cannot_read(monkeypatch, positions):
+    call = MropeCall(monkeypatch)
+    with pytest.raises(ValueError, match="positions"):
+        turn(positions, 7)
+    assert call.args is None
+
+
+@pytest.mark.parametrize("stride", [-1, 1, 6])
+def test_the_c_call_refuses_other_strides(stride):
+    from paper_2605_31598_gb300 import build_ext, statekv
+
+    build_ext.build()
+    fake = 1 << 20  # aligned, never touched
+    freq, axis = rotary.mrope_frequencies((16, 16), 1e4)
+    args = statekv.statekv_mrope_args(7, 4, 2, 64, 2, 32, 0, 0, 1.0, freq.data_ptr(), axis.data_ptr(), fake, stride,
+                                      fake, fake, fake, fake, 256, 128, 256, 128)
+    assert statekv.statekv_mrope(args, 0) == 1
