@@ -840,6 +840,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
+// A record of the kernel before.  The join is launched while that kernel runs, so the
+// words are not read-only for its whole life: a plain load, and it stays behind pdl_wait().
+__device__ __forceinline__ int4 read_record(const int4* at)
+{
+    int4 x;
+    asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(at) : "memory");
+    return x;
+}
+
 // Joins the shared tile that began with CTA blockIdx.x (kFew: tile blockIdx.x, if it is
 // shared), 16 rows of it: weights l_c 2^(ref_c - M) of the shares, in the order of the
 // keys; one pass with kAhead shares under way.  kFew is for tiles of four shares and
@@ -861,7 +870,7 @@ __global__ void __launch_bounds__(16 * D / 4) qcache_join(const __grid_constant_
         if (threadIdx.x == 0) found[1] = -1;
         __syncthreads();
         for (int c = threadIdx.x; c < p.ctas; c += blockDim.x) {
-            const int4 x = __ldg(p.starts + c);
+            const int4 x = read_record(p.starts + c);
             if (x.x == tile.x && x.y == tile.y && x.z == tile.z) {
                 found[0] = c;
                 found[1] = x.w;
@@ -872,7 +881,7 @@ __global__ void __launch_bounds__(16 * D / 4) qcache_join(const __grid_constant_
         cb = found[1];
         if (cb < 0) return;
     } else {
-        tile = __ldg(p.starts + ca);
+        tile = read_record(p.starts + ca);
         cb = tile.w;
         if (tile.x < 0) return;
     }

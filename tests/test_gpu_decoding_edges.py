@@ -28,3 +28,64 @@ def test_mrope_of_positions_expanded_over_the_axes(tokens, row, adjacent):
     want = mrope(q, k, at.contiguous(), freq, axis, adjacent=adjacent)
     got = mrope(q, k, at, freq, axis, adjacent=adjacent)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def filled_cache(S, L, H, d, capacity, block, held, seed):
+    """A cache with ``held`` rows of noise in every unit."""
+    from paper_2605_31598_gb300 import QCache
+
+    c = QCache(S, L, H, d, capacity, block_tokens=block)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    k, v = (torch.randn((S, L, held, H, d), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    assert c.append(k, v, torch.zeros((S, L), dtype=torch.int32, device="cuda")) == 0 and c.sync() == 0
+    return c
+
+
+def noise(shape, seed):
+    return torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").to(torch.bfloat16)
+
+
+def dequantised(c, held):
+    """K and V of the first ``held`` rows in 64 bits: [S][L][H][held][d]."""
+    return [getattr(c, x + "_codes").view(torch.float8_e4m3fn)[:, :, :, :held].double()
+            * getattr(c, x + "_scale").double().repeat_interleave(c.block_tokens, -1)[:, :, :, :held, None] for x in "kv"]
+
+
+def definition(q, k, v, start, scale=None):
+    """Causal attention in 64 bits of q [S][L][n][Hq][d] at rows start + i, and sum p |v|."""
+    S, L, n, Hq, d = q.shape
+    H, held = k.shape[2:4]
+    qq = q.double().view(S, L, n, H, Hq // H, d)
+    z = torch.einsum("slnhgd,slhjd->slnhgj", qq, k) * (d ** -0.5 if scale is None else scale)
+    lim = start.long()[:, :, None] + torch.arange(n, device=q.device)
+    z = z.masked_fill((torch.arange(held, device=q.device) > lim[..., None])[:, :, :, None, None], float("-inf"))
+    p = torch.softmax(z, -1)
+    return [torch.einsum("slnhgj,slhjd->slnhgd", p, x).reshape(q.shape) for x in (v, v.abs())]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("L,capacity", [(1, 20_480), (60, 3_072)])
+def test_calls_of_other_lengths_in_turn(d, L, capacity):
+    """160 query rows of a KV head over the same cache at lengths that change from call
+    to call, so the tiles that CTAs share change too, on one workspace and without a
+    wait between the calls: each gives what the definition says (one rounding to bf16,
+    weights in fp16), and the same bits every time."""
+    n, Hq, held = 40, 4, 3_000
+    c = filled_cache(1, L, 1, d, capacity, 64, held, seed=d + L)
+    q = noise((1, L, n, Hq, d), 5)
+    lengths = [held, 257, 1_500, 700, n]
+    starts = [torch.full((1, L), m - n, dtype=torch.int32, device="cuda") for m in lengths]
+    if L > 1:  # and lengths that differ between the units
+        starts.append((torch.arange(L, device="cuda", dtype=torch.int32) * 49)[None].contiguous())
+    outs = [[torch.zeros_like(q) for _ in range(12)] for _ in starts]
+    for i in range(12):
+        for st, out in zip(starts, outs):
+            assert c.attend(q, st, out[i]) == 0
+    assert c.sync() == 0
+    k, v = dequantised(c, held)
+    for st, out in zip(starts, outs):
+        for x in out[1:]:
+            assert torch.equal(x.view(torch.int16), out[0].view(torch.int16))
+        for l in range(0, L, 20):
+            want, size = definition(q[:, l:l + 1], k[:, l:l + 1], v[:, l:l + 1], st[:, l:l + 1])
+            assert ((out[0][:, l:l + 1].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -10 * size).all()
