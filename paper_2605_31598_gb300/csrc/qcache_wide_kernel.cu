@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     float* scales = reinterpret_cast<float*>(sm + L::kOffScale);
     uint32_t* misc = reinterpret_cast<uint32_t*>(sm + L::kOffMisc);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
-    volatile int* poison = reinterpret_cast<volatile int*>(misc + 4);
+    volatile int* poison = reinterpret_cast<volatile int*>(misc + 4);  // [8 tiles], a byte per converter warp
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cta = blockIdx.x;
 
@@ -462,6 +462,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;" ::: "memory");
         // -------------------------------------------------------------- converters
         const int key = threadIdx.x - 128;
+        // the warp's byte of each tile's poison word: the warps may be a step apart, so none
+        // clears what another has set
+        volatile uint8_t* mark = reinterpret_cast<volatile uint8_t*>(misc + 4) + (warp - 4);
         bool ok = true;
         int n = 0, step = 0, tiles = 0;  // raw tiles, steps, tiles with steps so far
         uint32_t gsteps0 = 0, gsteps1 = 0, gtiles0 = 0, gtiles1 = 0;  // steps and tiles of each half so far
@@ -482,7 +485,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             read_scales(seg.sa);
             float vref = 0.f, vinv = 0.f, vmax = 0.f;
             // the softmax warpgroups are fewer than eight tiles with steps behind
-            if (key == 0) poison[tiles & 7] = 0;
+            if (lane == 0) mark[4 * (tiles & 7)] = 0;
+            __syncwarp();
             for (int j = seg.sa; ok && j < t.s1; ++j, ++step) {
                 const int base = t.begin + j * kBK;
                 // the unit of O follows the step's V scale: up at once, down when the scale is
@@ -528,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 const uint32_t bad = __vcmpeq4(w[i] & 0x7f7f7f7fu, 0x7f7f7f7fu);
-                                if (keep && bad) poison[tiles & 7] = 1;
+                                if (keep && bad) mark[4 * (tiles & 7)] = 1;
                                 w[i] = keep ? w[i] & ~bad : 0u;
                             }
                         }

@@ -89,3 +89,25 @@ def test_calls_of_other_lengths_in_turn(d, L, capacity):
         for l in range(0, L, 20):
             want, size = definition(q[:, l:l + 1], k[:, l:l + 1], v[:, l:l + 1], st[:, l:l + 1])
             assert ((out[0][:, l:l + 1].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -10 * size).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_nan_row_reaches_its_queries_in_many_short_units(d):
+    """40 queries of one KV head in each of 400 units of 110 keys (a tile of one step
+    each), every unit with a NaN code in one of the rows that some queries see: exactly
+    those queries have it, in every call."""
+    L, n, held = 400, 40, 110
+    c = filled_cache(1, L, 1, d, 128, 16, held, seed=d)
+    unit = torch.arange(L, device="cuda")
+    row, place = held - n + 1 + unit % (n - 1), unit * 7 % d  # rows 71 .. 109
+    c.v_codes[0, unit, 0, row, place] = 0x7F
+    q = noise((1, L, n, 1, d), 3)
+    start = torch.full((1, L), held - n, dtype=torch.int32, device="cuda")
+    want = torch.zeros((1, L, n, 1, d), dtype=torch.bool, device="cuda")
+    sees = held - n + torch.arange(n, device="cuda")[None] >= row[:, None]
+    want[0, :, :, 0].scatter_(2, place[:, None, None].expand(L, n, 1), sees[..., None])
+    out = torch.empty_like(q)
+    for _ in range(20):
+        out.zero_()
+        assert c.attend(q, start, out) == 0 and c.sync() == 0
+        assert torch.equal(torch.isnan(out), want)
