@@ -690,10 +690,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int gr = 0; gr < 8; gr += 4) {
                         const float4 x = *reinterpret_cast<const float4*>(ss + gr);
-                        cs[gr] = qscale * x.x;  // positive
-                        cs[gr + 1] = qscale * x.y;
-                        cs[gr + 2] = qscale * x.z;
-                        cs[gr + 3] = qscale * x.w;
+                        // positive, also where a zero query meets a zero block: a masked score stays
+                        // -inf under it, and scores that small are 0 beside any reference
+                        cs[gr] = fmaxf(qscale * x.x, 0x1p-126f);
+                        cs[gr + 1] = fmaxf(qscale * x.y, 0x1p-126f);
+                        cs[gr + 2] = fmaxf(qscale * x.z, 0x1p-126f);
+                        cs[gr + 3] = fmaxf(qscale * x.w, 0x1p-126f);
                     }
                     const float2 bu = *reinterpret_cast<const float2*>(ss + 8);
                     float beta = bu.x;
