@@ -54,6 +54,7 @@ class QCache:
         # enough for a few query rows per KV head; the attention of more makes a larger one
         self.workspace = torch.zeros(self.workspace_bytes(1, H), dtype=torch.uint8,
                                      device=self.k_codes.device)
+        self._outgrown = []
         self._sizes = {}
         self._at = ctypes.addressof(self.c)
         self._append, self._pack_append = packed_call("statekv_qcache_append", statekv_qcache_append_args, "5i3P6q")
@@ -100,9 +101,10 @@ class QCache:
         if need is None:
             need = self._sizes[key] = self.workspace_bytes(key[2], key[3], key[0], key[1])
         if self.workspace.numel() < need:
-            st = stream or torch.cuda.current_stream()
-            self.workspace.record_stream(st)  # an earlier call may still use it
-            with torch.cuda.stream(st):
+            # graphs captured with the smaller one may replay at any time, so it stays (there are
+            # two sizes: of calls for the few-row kernel alone, and of the others)
+            self._outgrown.append(self.workspace)
+            with torch.cuda.stream(stream or torch.cuda.current_stream()):
                 self.workspace = torch.zeros(need, dtype=torch.uint8, device=q.device)
         return self.workspace
 
@@ -113,10 +115,8 @@ class QCache:
         cache into ``out`` (like q) and ``lse`` (fp32 [S_cnt][L_cnt][n][Hq], may be
         None).  ``first``: int32 [S][L], first visible row of each unit.
         ``workspace``: a uint8 device tensor of ``workspace_bytes``, zero before its
-        first use; by default the
-        cache's own, which calls on one stream share (calls that may overlap, and
-        captured ones that outlive a larger call, bring their own).  Returns the C
-        status."""
+        first use; by default the cache's own, which calls on one stream share (calls
+        that may overlap bring their own).  Returns the C status."""
         r = self._range(stream_begin, stream_count, layer_begin, layer_count)
         shape = q.shape
         S, L, n, Hq, d = shape
@@ -141,5 +141,6 @@ class QCache:
         After an expired wait the cache's own workspace is made usable again."""
         status = statekv_qcache_sync(self.c, raw_stream(stream, self.status))
         if STATUS_NAMES.get(status) == "STATEKV_ERR_DEVICE_TIMEOUT":
-            self.workspace.zero_()
+            for ws in (self.workspace, *self._outgrown):
+                ws.zero_()
         return status

@@ -1,10 +1,12 @@
 """What the Python entry points of the decoding operators pass to the C calls, and
 what they refuse, with stand-ins for device tensors: nothing is enqueued."""
+import contextlib
+
 import numpy as np
 import pytest
 import torch
 
-from paper_2605_31598_gb300 import rotary
+from paper_2605_31598_gb300 import qcache, rotary
 
 
 class OnDevice:
@@ -85,3 +87,29 @@ def test_the_c_call_refuses_other_strides(stride):
     args = statekv.statekv_mrope_args(7, 4, 2, 64, 2, 32, 0, 0, 1.0, freq.data_ptr(), axis.data_ptr(), fake, stride,
                                       fake, fake, fake, fake, 256, 128, 256, 128)
     assert statekv.statekv_mrope(args, 0) == 1
+
+
+def cache_of_stand_ins(monkeypatch, capturing=False):
+    """A QCache without buffers, whose calls need 100 bytes of workspace for a token and
+    1000 for more; memory comes from the CPU."""
+    c = qcache.QCache.__new__(qcache.QCache)
+    c.shape, c._sizes, c._outgrown = (2, 3, 4, 128), {}, []
+    c.workspace = torch.zeros(100, dtype=torch.uint8)
+    monkeypatch.setattr(c, "workspace_bytes", lambda n, hq, sc, lc: 100 if n == 1 else 1000, raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: None)
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda x, s: None)
+    return c
+
+
+def test_a_workspace_that_was_handed_out_stays(monkeypatch):
+    """A captured call holds its address: a larger call must not give the memory back."""
+    c = cache_of_stand_ins(monkeypatch)
+    q = torch.zeros(1)
+    at = c._own_workspace((2, 3, 1, 28), q, None).data_ptr()
+    large = c._own_workspace((2, 3, 9, 28), q, None)
+    assert large.numel() == 1000 and not large.any()
+    assert [x.data_ptr() for x in c._outgrown] == [at]
+    assert c._own_workspace((2, 3, 9, 28), q, None) is large and c._own_workspace((2, 3, 1, 28), q, None) is large
+    assert len(c._outgrown) == 1  # and no more of them, however often calls alternate

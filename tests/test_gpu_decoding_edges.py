@@ -111,3 +111,32 @@ def test_a_nan_row_reaches_its_queries_in_many_short_units(d):
         out.zero_()
         assert c.attend(q, start, out) == 0 and c.sync() == 0
         assert torch.equal(torch.isnan(out), want)
+
+
+def test_a_captured_step_outlives_a_larger_call():
+    """A token step captured with the cache's own workspace, then a prompt that needs a
+    larger one: the graph still has its memory, and writes to nobody else's."""
+    L, H, Hq, d, held = 4, 4, 28, 128, 3_000
+    c = filled_cache(1, L, H, d, 16_384, 64, held, seed=9)
+    small = c.workspace.numel()
+    q, start = noise((1, L, 1, Hq, d), 1), torch.full((1, L), held - 1, dtype=torch.int32, device="cuda")
+    out = torch.zeros_like(q)
+    assert c.attend(q, start, out) == 0 and c.sync() == 0
+    want = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        assert c.attend(q, start, out) == 0
+    prompt = noise((1, L, 60, Hq, d), 2)
+    begin = start - 59
+    first = torch.zeros_like(prompt)
+    assert c.attend(prompt, begin, first) == 0 and c.sync() == 0
+    assert c.workspace.numel() > small
+    mine = [torch.full((small,), 7, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        again = torch.zeros_like(prompt)
+        assert c.attend(prompt, begin, again) == 0 and c.sync() == 0
+        assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+        assert torch.equal(again.view(torch.int16), first.view(torch.int16))
+    assert all(bool((x == 7).all()) for x in mine)
