@@ -10,6 +10,7 @@ from .statekv import (STATUS_NAMES, check, packed_call, raw_stream, statekv_qcac
                       statekv_qcache_attend_args, statekv_qcache_init, statekv_qcache_sync,
                       statekv_qcache_workspace_bytes)
 
+COUNTER_BYTES = 4096  # of a workspace, zero before its first use
 BUFFERS = ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail")
 
 
@@ -101,10 +102,15 @@ class QCache:
         if need is None:
             need = self._sizes[key] = self.workspace_bytes(key[2], key[3], key[0], key[1])
         if self.workspace.numel() < need:
-            # graphs captured with the smaller one may replay at any time, so it stays (there are
-            # two sizes: of calls for the few-row kernel alone, and of the others)
-            self._outgrown.append(self.workspace)
             with torch.cuda.stream(stream or torch.cuda.current_stream()):
+                if torch.cuda.is_current_stream_capturing():
+                    # memory of the graph, zeroed at each replay only: this call's and no other's
+                    ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+                    ws[:COUNTER_BYTES].zero_()
+                    return ws
+                # graphs captured with the smaller one may replay at any time, so it stays (there are
+                # two sizes: of calls for the few-row kernel alone, and of the others)
+                self._outgrown.append(self.workspace)
                 self.workspace = torch.zeros(need, dtype=torch.uint8, device=q.device)
         return self.workspace
 
@@ -116,7 +122,10 @@ class QCache:
         None).  ``first``: int32 [S][L], first visible row of each unit.
         ``workspace``: a uint8 device tensor of ``workspace_bytes``, zero before its
         first use; by default the cache's own, which calls on one stream share (calls
-        that may overlap bring their own).  Returns the C status."""
+        that may overlap bring their own).  A captured call that needs a larger one than
+        the cache has by then takes it from the graph's memory, with a node that zeroes
+        its counters: a call of its size beforehand, or ``workspace``, saves that.
+        Returns the C status."""
         r = self._range(stream_begin, stream_count, layer_begin, layer_count)
         shape = q.shape
         S, L, n, Hq, d = shape

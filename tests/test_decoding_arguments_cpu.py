@@ -113,3 +113,16 @@ def test_a_workspace_that_was_handed_out_stays(monkeypatch):
     assert [x.data_ptr() for x in c._outgrown] == [at]
     assert c._own_workspace((2, 3, 9, 28), q, None) is large and c._own_workspace((2, 3, 1, 28), q, None) is large
     assert len(c._outgrown) == 1  # and no more of them, however often calls alternate
+
+
+def test_a_capture_makes_no_workspace_for_later_calls(monkeypatch):
+    """What a capture zeroes is zero at a replay only, so no eager call may take it."""
+    c = cache_of_stand_ins(monkeypatch, capturing=True)
+    q, small = torch.zeros(1), c.workspace
+    assert c._own_workspace((2, 3, 1, 28), q, None) is small
+    large = c._own_workspace((2, 3, 9, 28), q, None)
+    assert large.numel() == 1000 and not large[:4096].any()
+    assert c.workspace is small and not c._outgrown
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    eager = c._own_workspace((2, 3, 9, 28), q, None)
+    assert eager is c.workspace and eager is not large and not eager.any()

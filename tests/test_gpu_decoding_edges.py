@@ -140,3 +140,32 @@ def test_a_captured_step_outlives_a_larger_call():
         assert torch.equal(out.view(torch.int16), want.view(torch.int16))
         assert torch.equal(again.view(torch.int16), first.view(torch.int16))
     assert all(bool((x == 7).all()) for x in mine)
+
+
+def test_a_prompt_whose_first_call_is_captured():
+    """Two layers' attention captured before any call of their size; an eager call comes
+    before the first replay, and others between the replays."""
+    L, H, Hq, d, held, n = 2, 2, 14, 128, 3_000, 60
+    c = filled_cache(1, L, H, d, 65_536, 64, held, seed=19)
+    assert c.workspace_bytes(n, Hq, 1, 1) > c.workspace.numel()
+    q = noise((1, L, n, Hq, d), 1)
+    parts = [q[:, l:l + 1].contiguous() for l in range(L)]
+    outs = [torch.zeros_like(x) for x in parts]
+    start = torch.full((1, L), held - n, dtype=torch.int32, device="cuda")
+    k, v = dequantised(c, held)
+    want, size = definition(q, k, v, start)
+    dirty = [torch.full((c.workspace_bytes(n, Hq, 1, 1),), 0x55, dtype=torch.uint8, device="cuda") for _ in range(3)]
+    del dirty  # what the allocator hands out next is not zero
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for l in range(L):
+            assert c.attend(parts[l], start, outs[l], layer_begin=l, layer_count=1) == 0
+    for turn in range(3):
+        eager = torch.zeros_like(q)
+        assert c.attend(q, start, eager) == 0 and c.sync() == 0
+        for x in outs:
+            x.zero_()
+        graph.replay()
+        assert c.sync() == 0
+        for got in (eager, torch.cat(outs, 1)):
+            assert ((got.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -10 * size).all(), turn
