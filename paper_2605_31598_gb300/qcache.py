@@ -147,9 +147,11 @@ class QCache:
 
     def sync(self, stream=None) -> int:
         """Synchronise and return what the kernels recorded (statekv_qcache_sync).
-        After an expired wait the cache's own workspace is made usable again."""
+        After an expired wait the cache's own workspaces are made usable again, for that
+        stream's next calls."""
         status = statekv_qcache_sync(self.c, raw_stream(stream, self.status))
         if STATUS_NAMES.get(status) == "STATEKV_ERR_DEVICE_TIMEOUT":
-            for ws in (self.workspace, *self._outgrown):
-                ws.zero_()
+            with torch.cuda.stream(stream or torch.cuda.current_stream()):
+                for ws in (self.workspace, *self._outgrown):
+                    ws[:COUNTER_BYTES].zero_()
         return status

@@ -169,3 +169,39 @@ def test_a_prompt_whose_first_call_is_captured():
         assert c.sync() == 0
         for got in (eager, torch.cat(outs, 1)):
             assert ((got.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -10 * size).all(), turn
+
+
+def test_after_an_expired_wait_the_workspaces_are_usable_on_the_stream_given(monkeypatch):
+    """``sync`` of a stream that reports an expired wait zeroes the counters before
+    that stream's next call, whatever the current stream is doing."""
+    from paper_2605_31598_gb300 import qcache
+
+    c = filled_cache(1, 1, 4, 128, 16_384, 64, 3_000, seed=29)
+    side = torch.cuda.Stream()
+    token, prompt = noise((1, 1, 1, 28, 128), 1), noise((1, 1, 60, 28, 128), 2)
+    start = torch.full((1, 1), 2_940, dtype=torch.int32, device="cuda")
+    calls = [(x, start + 60 - x.shape[2]) for x in (token, prompt)]
+    want = [torch.zeros_like(x) for x, _ in calls]
+    spaces = []
+    for (x, st), out in zip(calls, want):
+        assert c.attend(x, st, out) == 0 and c.sync() == 0
+        spaces.append(c.workspace)
+    assert spaces[0] is not spaces[1]
+    real = qcache.statekv_qcache_sync
+    monkeypatch.setattr(qcache, "statekv_qcache_sync", lambda *a: real(*a) or 5)  # DEVICE_TIMEOUT
+    got = [torch.zeros_like(x) for x, _ in calls]
+    for ws in spaces:
+        ws[:4096] = 1  # as a call that stopped halfway may leave it
+    torch.cuda.synchronize()
+    torch.cuda._sleep(400_000_000)
+    assert c.sync(side) == 5
+    with torch.cuda.stream(side):
+        seen = [ws[:4096].cpu() for ws in spaces]
+    assert not any(x.any() for x in seen)
+    monkeypatch.undo()
+    for (x, st), out in zip(calls, got):
+        assert c.attend(x, st, out, stream=side) == 0
+    assert c.sync(side) == 0
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
