@@ -60,6 +60,8 @@ class QCache:
         self._at = ctypes.addressof(self.c)
         self._append, self._pack_append = packed_call("statekv_qcache_append", statekv_qcache_append_args, "5i3P6q")
         self._attend, self._pack_attend = packed_call("statekv_qcache_attend", statekv_qcache_attend_args, "7if6PN")
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()  # what is zeroed here is zero for calls on any stream
 
     def _range(self, stream_begin, stream_count, layer_begin, layer_count):
         S, L = self.shape[:2]

@@ -205,3 +205,24 @@ def test_after_an_expired_wait_the_workspaces_are_usable_on_the_stream_given(mon
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+def test_a_new_cache_is_ready_for_every_stream():
+    """The counters and the status word of a cache made while its stream is busy are zero
+    for a stream that does not wait for it."""
+    from paper_2605_31598_gb300 import QCache
+
+    side = torch.cuda.Stream()
+    sizes = [(1, 1, 1, 64, 64), (1, 1, 4, 128, 256)]
+    for S, L, H, d, cap in sizes:
+        nbytes = QCache(S, L, H, d, cap).workspace.numel()
+        dirty = [torch.full((nbytes,), 0x55, dtype=torch.uint8, device="cuda") for _ in range(3)]
+        word = [torch.full((1,), 3, dtype=torch.int32, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        del dirty, word
+        torch.cuda._sleep(400_000_000)  # a fifth of a second
+        c = QCache(S, L, H, d, cap)
+        with torch.cuda.stream(side):
+            seen = c.workspace[:4096].cpu(), c.status.cpu()
+        assert not seen[0].any() and not seen[1].any()
+        torch.cuda.synchronize()
