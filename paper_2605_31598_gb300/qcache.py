@@ -40,10 +40,14 @@ class QCache:
         if tensors is None:
             tensors = {x: torch.zeros(shapes[x[2:]], dtype=types[x[2:]][0], device=device)
                        for x in BUFFERS}
+        self.device = tensors[BUFFERS[0]].get_device()
+        if self.device < 0 or self.device != torch.cuda.current_device():
+            raise ValueError("the cache's device has to be the current one (torch.cuda.device)")
         for x in BUFFERS:
             t = tensors[x]
-            if t.shape != shapes[x[2:]] or t.dtype not in types[x[2:]] or not t.is_contiguous() or not t.is_cuda:
-                raise ValueError(f"{x}: a contiguous {types[x[2:]][0]} device tensor {shapes[x[2:]]}")
+            if t.shape != shapes[x[2:]] or t.dtype not in types[x[2:]] or not t.is_contiguous() or \
+                    t.get_device() != self.device:
+                raise ValueError(f"{x}: a contiguous {types[x[2:]][0]} tensor {shapes[x[2:]]} on the cache's device")
             setattr(self, x, t)
         self.shape = (S, L, H, d)
         self.capacity, self.block_tokens = capacity, b
@@ -69,8 +73,9 @@ class QCache:
                 layer_begin, L - layer_begin if layer_count is None else layer_count)
 
     def _units(self, x, name):
-        if x.dtype != torch.int32 or x.shape != self.shape[:2] or not x.is_contiguous() or not x.is_cuda:
-            raise ValueError(f"{name}: a contiguous int32 device tensor {self.shape[:2]}")
+        if x.dtype != torch.int32 or x.shape != self.shape[:2] or not x.is_contiguous() or \
+                x.get_device() != self.device:
+            raise ValueError(f"{name}: a contiguous int32 tensor {self.shape[:2]} on the cache's device")
         return x.data_ptr()
 
     def append(self, k, v, start, *, stream_begin=0, stream_count=None, layer_begin=0,
@@ -89,9 +94,9 @@ class QCache:
         one only: its stride may be anything)."""
         st = x.stride()
         if x.shape != (r[1], r[3], n, self.shape[2], self.shape[3]) or x.dtype != torch.bfloat16 or \
-                st[4] != 1 or not x.is_cuda or (r[1] > 1 and r[3] > 1 and st[0] != r[3] * st[1]):
-            raise ValueError(f"{name}: a bf16 device tensor [streams][layers][n][heads][d], its rows "
-                             "contiguous and its units evenly spaced")
+                st[4] != 1 or x.get_device() != self.device or (r[1] > 1 and r[3] > 1 and st[0] != r[3] * st[1]):
+            raise ValueError(f"{name}: a bf16 tensor [streams][layers][n][heads][d] on the cache's device, its "
+                             "rows contiguous and its units evenly spaced")
         return (st[1] if r[3] > 1 else st[0] if r[1] > 1 else 0, st[2] if n > 1 else 0,
                 st[3] if self.shape[2] > 1 else 0)
 
@@ -133,19 +138,20 @@ class QCache:
         S, L, n, Hq, d = shape
         if (q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or out.shape != shape
                 or not q.is_contiguous() or not out.is_contiguous() or S != r[1] or L != r[3]
-                or d != self.shape[3] or not q.is_cuda or not out.is_cuda):
-            raise ValueError("q, out: contiguous bf16 device tensors [streams][layers][n][heads][d]")
+                or d != self.shape[3] or q.get_device() != self.device or out.get_device() != self.device):
+            raise ValueError("q, out: contiguous bf16 tensors [streams][layers][n][heads][d] on the cache's device")
         if lse is not None and (lse.dtype != torch.float32 or lse.shape != shape[:4]
-                                or not lse.is_contiguous() or not lse.is_cuda):
-            raise ValueError("lse: a contiguous fp32 device tensor [streams][layers][n][heads]")
+                                or not lse.is_contiguous() or lse.get_device() != self.device):
+            raise ValueError("lse: a contiguous fp32 tensor [streams][layers][n][heads] on the cache's device")
+        handle = raw_stream(stream, q)
         ws = self._own_workspace((S, L, n, Hq), q, stream) if workspace is None else workspace
-        if ws.dtype != torch.uint8 or not ws.is_contiguous() or not ws.is_cuda:
-            raise ValueError("workspace: a contiguous uint8 device tensor")
+        if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.get_device() != self.device:
+            raise ValueError("workspace: a contiguous uint8 tensor on the cache's device")
         args = self._pack_attend(
             *r, n, Hq, causal, softmax_scale, self._units(start, "start"),
             0 if first is None else self._units(first, "first"), q.data_ptr(), out.data_ptr(),
             0 if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel())
-        return self._attend(self._at, args, raw_stream(stream, q))
+        return self._attend(self._at, args, handle)
 
     def sync(self, stream=None) -> int:
         """Synchronise and return what the kernels recorded (statekv_qcache_sync).

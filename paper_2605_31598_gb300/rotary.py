@@ -37,13 +37,14 @@ def _call():
     return packed_call("statekv_mrope", statekv_mrope_args, "8if3Pq4P4q")
 
 
-def _rows(x, tokens, heads, d, name):
+def _rows(x, tokens, heads, d, device, name):
     """Elements between the tokens of x, which has to be bf16 [tokens][heads][d] on
-    the device with contiguous tokens."""
+    the positions' device with contiguous tokens."""
     st = x.stride()
     if x.dtype != torch.bfloat16 or x.shape != (tokens, heads, d) or st[2] != 1 or \
-            (st[1] != d and heads > 1) or not x.is_cuda:
-        raise ValueError(f"{name}: a bf16 device tensor {(tokens, heads, d)} whose tokens are contiguous rows")
+            (st[1] != d and heads > 1) or x.get_device() != device:
+        raise ValueError(f"{name}: a bf16 tensor {(tokens, heads, d)} on the positions' device whose tokens are "
+                         "contiguous rows")
     return st[0] if tokens > 1 else heads * d
 
 
@@ -63,7 +64,8 @@ def mrope(q, k, positions, freq, axis, *, scale=1.0, adjacent=False, transpose=F
     if freq.dtype != torch.float64 or axis.dtype != torch.int32 or axis.numel() != pairs or \
             freq.is_cuda or axis.is_cuda or not freq.is_contiguous() or not axis.is_contiguous():
         raise ValueError("freq and axis: contiguous CPU tensors, fp64 and int32, one entry per pair")
-    if positions.dtype != torch.int32 or width < tokens or (ps[1] != 1 and width > 1) or not positions.is_cuda:
+    device = positions.get_device()  # -1: not a device tensor
+    if positions.dtype != torch.int32 or width < tokens or (ps[1] != 1 and width > 1) or device < 0:
         raise ValueError("positions: an int32 device tensor [axes][tokens]")
     axis_stride = ps[0] if axes > 1 else width  # of one axis it has no meaning
     if 0 < axis_stride < tokens:
@@ -71,21 +73,21 @@ def mrope(q, k, positions, freq, axis, *, scale=1.0, adjacent=False, transpose=F
     hq = hk = q_ptr = k_ptr = qo_ptr = ko_ptr = qs = ks = qos = kos = 0
     if q is not None:
         hq = q.shape[1]
-        qs = _rows(q, tokens, hq, d, "q")
+        qs = _rows(q, tokens, hq, d, device, "q")
         if q_out is None:
             q_out, qos = torch.empty((tokens, hq, d), dtype=torch.bfloat16, device=q.device), hq * d
         else:
-            qos = _rows(q_out, tokens, hq, d, "q_out")
+            qos = _rows(q_out, tokens, hq, d, device, "q_out")
         q_ptr, qo_ptr = q.data_ptr(), q_out.data_ptr()
     if k is not None:
         hk = k.shape[1]
         if k.shape[0] != tokens or k.shape[2] != d:
             raise ValueError("k: other tokens or another head dim than q")
-        ks = _rows(k, tokens, hk, d, "k")
+        ks = _rows(k, tokens, hk, d, device, "k")
         if k_out is None:
             k_out, kos = torch.empty((tokens, hk, d), dtype=torch.bfloat16, device=k.device), hk * d
         else:
-            kos = _rows(k_out, tokens, hk, d, "k_out")
+            kos = _rows(k_out, tokens, hk, d, device, "k_out")
         k_ptr, ko_ptr = k.data_ptr(), k_out.data_ptr()
     call, pack = _call()
     check(call(pack(tokens, hq, hk, d, axes, pairs, adjacent, transpose, scale, freq.data_ptr(), axis.data_ptr(),

@@ -93,7 +93,7 @@ def cache_of_stand_ins(monkeypatch, capturing=False):
     """A QCache without buffers, whose calls need 100 bytes of workspace for a token and
     1000 for more; memory comes from the CPU."""
     c = qcache.QCache.__new__(qcache.QCache)
-    c.shape, c._sizes, c._outgrown = (2, 3, 4, 128), {}, []
+    c.shape, c.device, c._sizes, c._outgrown = (2, 3, 4, 128), 0, {}, []
     c.workspace = torch.zeros(100, dtype=torch.uint8)
     monkeypatch.setattr(c, "workspace_bytes", lambda n, hq, sc, lc: 100 if n == 1 else 1000, raising=False)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: None)
@@ -126,3 +126,94 @@ def test_a_capture_makes_no_workspace_for_later_calls(monkeypatch):
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     eager = c._own_workspace((2, 3, 9, 28), q, None)
     assert eager is c.workspace and eager is not large and not eager.any()
+
+
+class CacheCalls:
+    """The C calls of a cache of stand-ins; counts what gets that far."""
+
+    def __init__(self, monkeypatch, device=0, current=0):
+        self.cache, self.device, self.calls = cache_of_stand_ins(monkeypatch), device, 0
+        c = self.cache
+        c.device, c._at = device, 0
+        c._append = c._attend = self.call
+        c._pack_append = c._pack_attend = lambda *fields: fields
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current, raising=False)
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 0, raising=False)
+
+    def call(self, *args):
+        self.calls += 1
+        return 0
+
+    def tensors(self, elsewhere=None):
+        """A call's tensors on the cache's device, but for one."""
+        def on(name, x):
+            return OnDevice(x, self.device + (name == elsewhere))
+
+        rows = {x: on(x, torch.zeros((2, 3, 5, h, 128), dtype=torch.bfloat16))
+                for x, h in (("q", 28), ("out", 28), ("k", 4), ("v", 4))}
+        units = {x: on(x, torch.zeros((2, 3), dtype=torch.int32)) for x in ("start", "first")}
+        return dict(rows, **units, lse=on("lse", torch.zeros((2, 3, 5, 28))),
+                    workspace=on("workspace", torch.zeros(2000, dtype=torch.uint8)))
+
+    def append(self, t, **kw):
+        return self.cache.append(t["k"], t["v"], t["start"], **kw)
+
+    def attend(self, t, **kw):
+        return self.cache.attend(t["q"], t["start"], t["out"], lse=t["lse"], first=t["first"], workspace=t["workspace"], **kw)
+
+
+class OtherStream:
+    device_index, cuda_stream = 1, 0
+
+
+def test_a_cache_takes_tensors_of_its_device_only(monkeypatch):
+    c = CacheCalls(monkeypatch)
+    assert c.append(c.tensors()) == 0 and c.attend(c.tensors()) == 0 and c.calls == 2
+    for call, names in ((c.append, ("k", "v", "start")), (c.attend, ("q", "out", "lse", "start", "first", "workspace"))):
+        for name in names:
+            with pytest.raises(ValueError, match="device"):
+                call(c.tensors(elsewhere=name))
+        with pytest.raises(ValueError, match="device"):
+            call(c.tensors(), stream=OtherStream)
+    assert c.calls == 2
+
+
+def test_the_device_of_a_cache_has_to_be_current(monkeypatch):
+    c = CacheCalls(monkeypatch, device=1, current=0)
+    for call in (c.append, c.attend):
+        with pytest.raises(ValueError, match="current"):
+            call(c.tensors())
+    assert c.calls == 0
+    # nor is a cache made there: kernels are prepared, and the workspace sized, for the current device
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(qcache, "statekv_qcache_init", lambda c: pytest.fail("a cache elsewhere was prepared"))
+    shapes = {"codes": ((1, 1, 1, 16, 64), torch.uint8), "scale": ((1, 1, 1, 1), torch.float32),
+              "tail": ((1, 1, 1, 16, 64), torch.bfloat16)}
+    for devices in ({}, {"k_codes": 0, "v_codes": 0}):  # all on device 1, and some
+        buffers = {x: OnDevice(torch.zeros(shapes[x[2:]][0], dtype=shapes[x[2:]][1]), devices.get(x, 1)) for x in qcache.BUFFERS}
+        with pytest.raises(ValueError, match="device"):
+            qcache.QCache(1, 1, 1, 64, 16, block_tokens=16, tensors=buffers)
+
+
+@pytest.mark.parametrize("devices,stream", [
+    (dict(q=1), None), (dict(k=1), None), (dict(positions=1), None), (dict(q_out=1), None), (dict(k_out=1), None),
+    (dict(q=1, k=1, positions=1, q_out=1, k_out=1), None),  # together, but elsewhere than the launch
+    (dict(), OtherStream),
+])
+def test_mrope_takes_tensors_of_the_current_device_only(monkeypatch, devices, stream):
+    called = []
+    monkeypatch.setattr(rotary, "_call", lambda: (lambda args, stream: called.append(args) or 0, lambda *fields: fields))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 0, raising=False)
+    freq, axis = rotary.mrope_frequencies((8, 12, 12), 1e4)
+
+    def call(devices, stream):
+        t = {x: OnDevice(torch.zeros((7, 2, 64), dtype=torch.bfloat16), devices.get(x, 0)) for x in ("q", "k", "q_out", "k_out")}
+        at = OnDevice(torch.zeros((3, 7), dtype=torch.int32), devices.get("positions", 0))
+        rotary.mrope(t["q"], t["k"], at, freq, axis, q_out=t["q_out"], k_out=t["k_out"], stream=stream)
+
+    call({}, None)
+    assert len(called) == 1
+    with pytest.raises(ValueError, match="device"):
+        call(devices, stream)
+    assert len(called) == 1
