@@ -577,7 +577,10 @@ statekv_status statekv_qcache_append(const statekv_qcache* cache,
  * calls of more than 32 query rows per KV head, so is a V element times its
  * block's scale over a common one: exact for power-of-two scales up to 2^15
  * apart).  So a key's share of a sum is kept to 2^-11 of itself or 2^-22 of its
- * row's largest weight times the largest V block scale, whichever is larger.
+ * row's largest weight times the largest V block scale, whichever is larger.  In those
+ * calls, at head_dim 128, a q element below 2^-13 of its row's largest is kept to 2^-21
+ * of that; every other enters the scores as it is (in all other calls, from 2^-32 of the
+ * row's largest on; smaller ones are kept to 2^-39 of it).
  * Results do not depend on timing: the same call on the same cache gives the same
  * bits.
  * INVALID_ARG for bad arguments or a workspace that is too small; UNSUPPORTED for

@@ -7,11 +7,14 @@
 //
 // Per step the codes of 128 K rows and 128 V rows arrive by TMA (16 KB each, D =
 // 128), and both halves use them.
-//   S = Q K^T  D = 128: on the codes as they are (kind::f8f6f4).  A bf16 query
-//     element, scaled by its row's power of two, is the sum of two e4m3 numbers, its
-//     first four significant bits and the rest, exactly down to 2^-10 of the row's
-//     largest (and to 2^-18 of it below): two products at twice the fp16 rate.  D =
-//     64 (two keys to a 128-byte row): K codes are turned into fp16 like V's.
+//   S = Q K^T  D = 128: on the codes as they are (kind::f8f6f4).  A row of
+//     queries is scaled by the power of two that brings its largest element into [2^7,
+//     2^8).  A bf16 element is then the sum of an e4m3 number, its first four significant
+//     bits, and an e5m2 number, the rest: at most eight units of its last place, which
+//     three bits hold.  Exactly so down to 2^-13 of the row's largest, where the first
+//     part gets coarse; below, the sum is within 2^-21 of the largest (2^-17 if the rest
+//     were e4m3 too).  Two products at twice the fp16 rate.  D = 64 (two keys to a
+//     128-byte row): K codes are turned into fp16 like V's.
 //   O += P V  P over S in TMEM; V's codes are turned into fp16 tiles in shared
 //     memory by four converter warps.
 // Shared memory bounds the step: the products read 192 KB of operands for both
@@ -100,19 +103,29 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Instruction descriptor, fp32 D: kind::f16 with fp16 A/B, or kind::f8f6f4 with
+// e4m3 A/B (both formats have code 0).
+constexpr uint32_t idesc_of(int M, int N, bool b_mn_major)
+{
+    return (1u << 4) | (static_cast<uint32_t>(b_mn_major) << 16) | (static_cast<uint32_t>(N >> 3) << 17) |
+           (static_cast<uint32_t>(M >> 4) << 24);
+}
+constexpr uint32_t kE5m2A = 1u << 7;  // kind::f8f6f4: A in e5m2
+
 // Products of NK k steps, fp16 inputs, fp32 accumulator.  The descriptors come as
 // their 32-bit words and a step's offset goes onto the low one: the issuing warp
 // shares its scheduler with softmax and converter warps, so every instruction
 // beside the MMAs holds the tensor core up.
 // S = A[smem, K-major] * B[smem, K-major], 32 bytes of the k axis per step.  fp16: one
-// pass.  e4m3: A's two parts one after the other, 128 rows of 128 bytes each.
+// pass.  8 bits: A's two parts (e4m3, e5m2) one after the other, 128 rows of 128 bytes each.
 template <int D>
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t alo, uint32_t blo, uint32_t hi, uint32_t idesc)
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t alo, uint32_t blo, uint32_t hi, uint32_t idesc0)
 {
     constexpr bool kDirect = Layout<D>::kDirect;
     constexpr int NK = kDirect ? 2 * (D / 32) : D / 16;
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
+        const uint32_t idesc = kDirect && k >= 4 ? idesc0 | kE5m2A : idesc0;
         // 16 KB per 128 bytes of the k axis (an e4m3 part), 32 bytes per step inside
         const uint32_t a = alo + (((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4);
         const uint32_t b = kDirect ? blo + (((k & 3) * 32) >> 4) : blo + (((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4);
@@ -177,14 +190,6 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t blo, uin
     }
 }
 
-// Instruction descriptor, fp32 D: kind::f16 with fp16 A/B, or kind::f8f6f4 with
-// e4m3 A/B (both formats have code 0).
-constexpr uint32_t idesc_of(int M, int N, bool b_mn_major)
-{
-    return (1u << 4) | (static_cast<uint32_t>(b_mn_major) << 16) | (static_cast<uint32_t>(N >> 3) << 17) |
-           (static_cast<uint32_t>(M >> 4) << 24);
-}
-
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
 {
     asm volatile(
@@ -194,6 +199,14 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr)
         : "memory");
+}
+
+// two fp32 values -> two e5m2 codes, the first in the low byte
+__device__ __forceinline__ uint32_t e5m2x2(float lo, float hi)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
 }
 
 // Packed pair of floats in one 64-bit register (f32x2 arithmetic).
@@ -606,8 +619,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             float ref = -INFINITY, l = 0.f, vref = 0.f;
             const int lim = lim_of(p, t.sp, r);
             if (active && nt > 0) {
-                // Q row, scaled by a power of two: into [2^14, 2^15) as fp16, or [2^7, 2^8) as two
-                // e4m3 parts; K-major swizzled
+                // Q row, scaled by a power of two: into [2^14, 2^15) as fp16, or [2^7, 2^8) as an
+                // e4m3 and an e5m2 part; K-major swizzled
                 float qscale;
                 {
                     uint4 x[D / 8];
@@ -643,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                     const uint32_t code = e4m3x2(f[2 * b], f[2 * b + 1]);
                                     f16_of(code, a, g);  // the codes' values
                                     const float2 v2 = __half22float2(*reinterpret_cast<const __half2*>(&a));
-                                    l0 = e4m3x2(f[2 * b] - v2.x, f[2 * b + 1] - v2.y);
+                                    l0 = e5m2x2(f[2 * b] - v2.x, f[2 * b + 1] - v2.y);
                                     l1 = bad ? 0x7f7fu : code;
                                     part[0] |= l1 << (16 * b);
                                     part[1] |= l0 << (16 * b);

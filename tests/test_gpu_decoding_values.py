@@ -61,3 +61,54 @@ def test_zero_queries_and_zero_keys(d, rows):
         z = torch.where(some, seen.double().log(), float("-inf"))[None, None, :, None]
         assert torch.equal(lse.isinf(), z.isinf().expand(lse.shape))
         assert ((lse.double() - z).abs()[:, :, some] <= 2.0 ** -19 * z[:, :, some] + 2.0 ** -19).all()
+
+
+def outlier_queries(n, d, kind):
+    """Rows with one element far above the others."""
+    g = torch.Generator(device="cuda").manual_seed(n + d)
+    u = torch.rand((1, 1, n, 1, d), generator=g, device="cuda")
+    if kind == "small":    # all others at 2^-18 to 2^-17 of the largest's power of two, of one sign
+        q = (0.5 + 0.49 * u) * 2.0 ** -10
+        q[..., 0] = 192.0
+    else:                  # a thousand among 0.02 to 0.1
+        q = (0.02 + 0.08 * u) * torch.where(torch.rand(u.shape, generator=g, device="cuda") < 0.5, -1.0, 1.0)
+        q[..., 0] = 1000.0
+    return (q * torch.exp2(torch.arange(n, device="cuda") % 9 - 4.0)[:, None, None]).to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("kind", ["small", "mixed"])
+@pytest.mark.parametrize("d,rows", [(64, 1), (128, 1), (64, 40), (128, 40), (128, 300)])
+def test_queries_with_an_outlier(d, rows, kind):
+    """A query's small elements count beside a large one.  At d = 128 the tcgen05 kernel
+    takes Q as two 8-bit parts, off by 2^-21 of the row's largest element at most, so a
+    score is off by that times scale sum |k|: eps = 2^-20 + scale (d 2^-24 max sum |q k| +
+    2^-21 max |q| max sum |k|).  Keys have nothing at the outlier's place."""
+    from paper_2605_31598_gb300 import QCache
+
+    held = 400
+    c = QCache(1, 1, 1, d, wide_capacity(rows), block_tokens=16)
+    size = torch.linspace(0.5, 2.0, held, device="cuda")[:, None, None]
+    sign = torch.ones(d, device="cuda") if kind == "small" else torch.where(torch.arange(d, device="cuda") % 3 == 0, -1.0, 1.0)
+    k = (size * sign).expand(1, 1, held, 1, d).clone()
+    k[..., 0] = 0
+    v = torch.where(size > 1.25, 1.0, -1.0) * (1 + torch.arange(d, device="cuda") / d)
+    zero = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    assert c.append(k.to(torch.bfloat16), v.expand(1, 1, held, 1, d).to(torch.bfloat16), zero) == 0 and c.sync() == 0
+    q = outlier_queries(rows, d, kind)
+    kk, vv = dequantised(c, held)
+    start = zero + held - rows
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:4], device="cuda")
+    # a scale at which the small elements alone make scores of about one for the middle rows
+    scale = 2.0 ** 10 / d if kind == "small" else 0.25
+    assert c.attend(q, start, out, lse=lse, softmax_scale=scale) == 0 and c.sync() == 0
+    want, mag = definition(q, kk, vv, start, scale)
+    qq = q.double()[0, 0, :, 0]
+    z = qq @ kk[0, 0, 0].T * scale
+    lim = held - rows + torch.arange(rows, device="cuda")
+    hidden = torch.arange(held, device="cuda") > lim[:, None]
+    z = torch.logsumexp(z.masked_fill(hidden, float("-inf")), -1)
+    total = (qq.abs() @ kk[0, 0, 0].abs().T).amax(-1)
+    eps = 2.0 ** -20 + scale * (d * 2.0 ** -24 * total + 2.0 ** -21 * qq.abs().amax(-1) * kk.abs().sum(-1).max())
+    assert ((lse[0, 0, :, 0].double() - z).abs() <= eps + 2.0 ** -20 * z.abs()).all()
+    tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * eps[:, None, None]) * mag
+    assert ((out.double() - want).abs() <= tol).all()
