@@ -704,11 +704,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int gr = 0; gr < 8; gr += 4) {
                         const float4 x = *reinterpret_cast<const float4*>(ss + gr);
                         // positive, also where a zero query meets a zero block: a masked score stays
-                        // -inf under it, and scores that small are 0 beside any reference
-                        cs[gr] = fmaxf(qscale * x.x, 0x1p-126f);
-                        cs[gr + 1] = fmaxf(qscale * x.y, 0x1p-126f);
-                        cs[gr + 2] = fmaxf(qscale * x.z, 0x1p-126f);
-                        cs[gr + 3] = fmaxf(qscale * x.w, 0x1p-126f);
+                        // -inf under it (the addend rounds away beside a product from 2^-102 on, and
+                        // scores of smaller ones are 0 beside any reference)
+                        cs[gr] = fmaf(qscale, x.x, 0x1p-126f);
+                        cs[gr + 1] = fmaf(qscale, x.y, 0x1p-126f);
+                        cs[gr + 2] = fmaf(qscale, x.z, 0x1p-126f);
+                        cs[gr + 3] = fmaf(qscale, x.w, 0x1p-126f);
                     }
                     const float2 bu = *reinterpret_cast<const float2*>(ss + 8);
                     float beta = bu.x;
