@@ -48,6 +48,25 @@ def _rows(x, tokens, heads, d, device, name):
     return st[0] if tokens > 1 else heads * d
 
 
+class _Turn(torch.autograd.Function):
+    """``mrope`` and, as its gradient, the call that turns the other way."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, freq, axis, how, transpose, stream):
+        ctx.save_for_backward(positions, freq, axis)  # autograd refuses them once changed in place
+        ctx.set_materialize_grads(False)
+        ctx.how, ctx.transpose = how, transpose
+        return mrope(q, k, positions, freq, axis, transpose=transpose, stream=stream, **how)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        dq, dk = (x.contiguous() if x is not None and wanted else None
+                  for x, wanted in zip((dq, dk), ctx.needs_input_grad))
+        if dq is not None or dk is not None:
+            dq, dk = mrope(dq, dk, *ctx.saved_tensors, transpose=not ctx.transpose, **ctx.how)
+        return dq, dk, None, None, None, None, None, None
+
+
 def mrope(q, k, positions, freq, axis, *, scale=1.0, adjacent=False, transpose=False, q_out=None,
           k_out=None, stream=None):
     """q and k (bf16 [tokens][heads][d], the rows of a token contiguous; either may
@@ -55,10 +74,15 @@ def mrope(q, k, positions, freq, axis, *, scale=1.0, adjacent=False, transpose=F
     axes are equal, ``expand`` of one row will do); returns (q_out, k_out), made here
     unless given (``q_out=q`` turns in place).
     ``freq``, ``axis``: CPU tensors as from ``mrope_frequencies``.  ``transpose``
-    turns the other way: the gradient with respect to q and k.  Raises
-    StateKVError on a bad argument."""
+    turns the other way: the gradient with respect to q and k, which autograd forms
+    for those that require one (not with ``q_out`` or ``k_out``).  Raises StateKVError
+    on a bad argument."""
     if q is None and k is None:
         raise ValueError("q and k are both None")
+    if ((q is not None and q.requires_grad) or (k is not None and k.requires_grad)) and torch.is_grad_enabled():
+        if q_out is not None or k_out is not None:
+            raise ValueError("q_out, k_out: not for q or k that require a gradient")
+        return _Turn.apply(q, k, positions, freq, axis, dict(scale=scale, adjacent=adjacent), transpose, stream)
     tokens, _, d = (k if q is None else q).shape
     pairs, (axes, width), ps = freq.numel(), positions.shape, positions.stride()
     if freq.dtype != torch.float64 or axis.dtype != torch.int32 or axis.numel() != pairs or \
