@@ -528,7 +528,7 @@ statekv_status statekv_qcache_init(statekv_qcache* cache);
  * written.  A (stream, layer) whose rows would not fit is left as it is and the
  * status word records it (STATEKV_ERR_CACHE_FULL from statekv_qcache_sync).
  * The call does not advance start: append and attention of one step take the
- * same array.
+ * same array.  num_tokens = 0 is a no-op, here and in the attention.
  *   k, v  bf16, row i of head h of the ranges' unit u (stream-major) at
  *         u * unit + i * token + h * head elements of their strides; 16-byte
  *         aligned, strides non-negative multiples of 8

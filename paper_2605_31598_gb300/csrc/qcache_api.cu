@@ -186,8 +186,10 @@ statekv_status statekv_qcache_append(const statekv_qcache* c, const statekv_qcac
                                      statekv_stream stream)
 {
     if (!a || !prepared(c, nullptr) || !range_ok(*c, a->stream_begin, a->stream_count, a->layer_begin, a->layer_count) ||
-        a->num_tokens < 1 || a->num_tokens > c->capacity || !a->start || !aligned(a->start, 4))
+        a->num_tokens < 0 || a->num_tokens > c->capacity)
         return STATEKV_ERR_INVALID_ARG;
+    if (a->num_tokens == 0) return STATEKV_OK;
+    if (!a->start || !aligned(a->start, 4)) return STATEKV_ERR_INVALID_ARG;
     QAppendParams p{};
     const void* src[2] = {a->k, a->v};
     const statekv_qcache_strides* strides[2] = {&a->k_strides, &a->v_strides};
@@ -213,13 +215,13 @@ statekv_status statekv_qcache_append(const statekv_qcache* c, const statekv_qcac
 statekv_status statekv_qcache_workspace_bytes(const statekv_qcache* c, int32_t stream_count, int32_t layer_count,
                                               int32_t num_tokens, int32_t num_q_heads, size_t* bytes)
 {
-    if (!bytes || !prepared(c, nullptr) || !range_ok(*c, 0, stream_count, 0, layer_count) || num_tokens < 1 ||
+    if (!bytes || !prepared(c, nullptr) || !range_ok(*c, 0, stream_count, 0, layer_count) || num_tokens < 0 ||
         num_tokens > c->capacity || num_q_heads < 1 || num_q_heads % c->num_kv_heads != 0)
         return STATEKV_ERR_INVALID_ARG;
     const int G = num_q_heads / c->num_kv_heads;
     if (static_cast<long long>(num_tokens) * G > (1 << 24)) return STATEKV_ERR_UNSUPPORTED;
     const QAttendPlan plan = qcache_attend_plan(stream_count * layer_count, c->num_kv_heads, c->head_dim, c->capacity,
-                                                num_tokens, G, current_sm_count());
+                                                num_tokens > 0 ? num_tokens : 1, G, current_sm_count());
     if (!plan.fits) return STATEKV_ERR_UNSUPPORTED;
     *bytes = plan.bytes;
     return STATEKV_OK;
@@ -230,9 +232,12 @@ statekv_status statekv_qcache_attend(const statekv_qcache* c, const statekv_qcac
 {
     Prepared d;
     if (!a || !prepared(c, &d) || !range_ok(*c, a->stream_begin, a->stream_count, a->layer_begin, a->layer_count) ||
-        a->num_tokens < 1 || a->num_tokens > c->capacity || a->num_q_heads < 1 ||
+        a->num_tokens < 0 || a->num_tokens > c->capacity || a->num_q_heads < 1 ||
         a->num_q_heads % c->num_kv_heads != 0 || (a->causal != 0 && a->causal != 1) || !(a->softmax_scale >= 0.f) ||
-        !std::isfinite(a->softmax_scale) || !a->start || !aligned(a->start, 4) || !aligned(a->first, 4) || !a->q ||
+        !std::isfinite(a->softmax_scale))
+        return STATEKV_ERR_INVALID_ARG;
+    if (a->num_tokens == 0) return STATEKV_OK;
+    if (!a->start || !aligned(a->start, 4) || !aligned(a->first, 4) || !a->q ||
         !a->out || !aligned(a->q, 16) || !aligned(a->out, 16) || !aligned(a->lse, 4))
         return STATEKV_ERR_INVALID_ARG;
     const int G = a->num_q_heads / c->num_kv_heads;

@@ -226,3 +226,22 @@ def test_a_new_cache_is_ready_for_every_stream():
             seen = c.workspace[:4096].cpu(), c.status.cpu()
         assert not seen[0].any() and not seen[1].any()
         torch.cuda.synchronize()
+
+
+def test_a_step_of_no_tokens_does_nothing():
+    """As for ``mrope``: an empty call is no error, with or without a workspace."""
+    L, H, Hq, d, held = 2, 2, 4, 64, 100
+    c = filled_cache(1, L, H, d, 128, 32, held, seed=39)
+    before = [getattr(c, x).clone() for x in ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail")]
+    start = torch.full((1, L), held, dtype=torch.int32, device="cuda")
+    kv = torch.empty((1, L, 0, H, d), dtype=torch.bfloat16, device="cuda")
+    q = torch.empty((1, L, 0, Hq, d), dtype=torch.bfloat16, device="cuda")
+    assert c.workspace_bytes(0, Hq) == c.workspace_bytes(1, Hq)
+    ws = torch.zeros(c.workspace_bytes(0, Hq), dtype=torch.uint8, device="cuda")
+    assert c.append(kv, kv, start) == 0
+    assert c.attend(q, start, torch.empty_like(q)) == 0
+    assert c.attend(q, start, torch.empty_like(q), lse=torch.empty((1, L, 0, Hq), device="cuda"), workspace=ws) == 0
+    assert c.append(kv[:, :1], kv[:, :1], start, layer_begin=2, layer_count=1) == 1  # a range that is not there
+    assert c.sync() == 0
+    for x, y in zip(before, ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail")):
+        assert torch.equal(x.view(torch.uint8), getattr(c, y).view(torch.uint8))
