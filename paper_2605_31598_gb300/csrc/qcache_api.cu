@@ -10,6 +10,7 @@
 
 #include <atomic>
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 
 using namespace statekv;
@@ -263,6 +264,13 @@ statekv_status statekv_qcache_attend(const statekv_qcache* c, const statekv_qcac
     p.out = static_cast<__nv_bfloat16*>(a->out);
     p.lse = a->lse;
     p.watchdog_ns = kWaitNs;
+#if STATEKV_DEBUG_CHECKS
+    // for the test of what follows an expired wait: one is taken as run out, the others' limit is this
+    if (const char* ms = std::getenv("STATEKV_QCACHE_EXPIRE_MS")) {
+        p.expire = 1;
+        p.watchdog_ns = std::strtoull(ms, nullptr, 10) * 1000000ull;
+    }
+#endif
     return launch_qcache_attend(d.k, d.v, plan, p, static_cast<uint8_t*>(a->workspace),
                                 reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? STATEKV_OK : STATEKV_ERR_CUDA;
 }

@@ -36,6 +36,17 @@ __device__ __forceinline__ bool wait_full(uint64_t* bar, uint32_t parity, unsign
     }
 }
 
+// Debug builds can have a call's first CTA take one wait as run out, in the odd lanes of
+// each warp that comes by `there` (QAttendParams::expire).
+__device__ __forceinline__ bool expire_here(const QAttendParams& p, bool there)
+{
+#if STATEKV_DEBUG_CHECKS
+    return p.expire && there && blockIdx.x == 0 && (threadIdx.x & 1);
+#else
+    return false;
+#endif
+}
+
 __device__ __forceinline__ float ex2(float x)
 {
     float y;

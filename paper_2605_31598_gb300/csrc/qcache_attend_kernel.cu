@@ -250,7 +250,8 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
             if (it + kStages - 1 < count) load(it + kStages - 1);
             const float ks2[2] = {next[0], next[1]}, vs2[2] = {next[2], next[3]};
             read_scales(min(it + 1, count - 1));
-            ok = __all_sync(0xffffffffu, wait_full(&full[st], ((used + it) / kStages) & 1, p.watchdog_ns));
+            ok = __all_sync(0xffffffffu, wait_full(&full[st], ((used + it) / kStages) & 1, p.watchdog_ns) &&
+                                             !expire_here(p, warp == 0 && used + it == 1));
             if (!ok) break;
             const uint8_t* ks = ring + st * L::kStage;
             const uint8_t* vs = ks + L::kMat;

@@ -524,12 +524,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int v = 0; v < 2; ++v) {
                     const bool direct = L::kDirect && v == 0;
                     const int raw = n % kVRaw;
-                    if (direct) {
-                        // K's codes are used as they are: the warp only passes their arrival on
-                        ok = wait(&k_full[step % kKTiles], (step / kKTiles) & 1);
-                    } else {
-                        ok = wait(&raw_full[raw], (n / kVRaw) & 1);
-                    }
+                    // K's codes are used as they are: the warp only passes their arrival on
+                    bool there = direct ? wait(&k_full[step % kKTiles], (step / kKTiles) & 1)
+                                        : wait(&raw_full[raw], (n / kVRaw) & 1);
+                    if (expire_here(p, step == 1)) there = false;
+                    // one verdict for the warp: a lane that gave up alone would be missed at the next __syncwarp
+                    ok = __all_sync(0xffffffffu, there);
                     if (!ok) break;
                     if (!direct) {
                     const uint8_t* src = sRaw + raw * L::kRawBytes;
@@ -551,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                     const int slots = v ? kConvTiles : kKTiles, slot = step % slots, use = step / slots;
-                    ok = use == 0 || wait(v ? &v_empty[slot] : &k_empty[slot], (use - 1) & 1);
+                    ok = __all_sync(0xffffffffu, use == 0 || wait(v ? &v_empty[slot] : &k_empty[slot], (use - 1) & 1));
                     if (!ok) break;
                     uint8_t* dst = v ? sV + slot * L::kF16Bytes : sK + slot * L::kKBytes;
 #pragma unroll

@@ -374,6 +374,7 @@ struct QAttendParams {
     float* part_ml;          // [2 * ctas][tile_rows][2]
     int4* starts;            // [ctas] wide: unit, KV head, first row and last CTA of the shared tile that begins there
     unsigned long long watchdog_ns;
+    int expire;              // debug builds: take a wait of the first CTA as run out
 };
 // Units of one launch (a call with more is cut).  Query rows of a KV head in a tile of
 // the warp-level kernel, and of the tcgen05 kernel; the former takes up to kQCacheFewRows
