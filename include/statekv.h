@@ -561,7 +561,8 @@ statekv_status statekv_qcache_append(const statekv_qcache* cache,
  *   o_i = sum_j softmax_j(softmax_scale * q_i . k_j) v_j,   lse_i = log of the
  *   softmax's denominator.
  * A query that sees no row (start < 0, first beyond it, or rows beyond the
- * capacity, which the status word records) gets o = 0 and lse = -inf.  Rows that
+ * capacity, which the status word records) gets o = 0 and lse = -inf; one that sees
+ * rows and has an infinity or a NaN in it gets NaN.  Rows that
  * no query of the call sees are never used, whatever they hold.
  *   start, first  int32 [S][L] of the whole cache (device); first may be NULL (0)
  *   q     bf16 [S_cnt][L_cnt][num_tokens][Hq][d] (device, 16-byte aligned)

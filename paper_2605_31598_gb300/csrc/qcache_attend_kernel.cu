@@ -198,7 +198,8 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const int e = min(254, max(15, static_cast<int>(top >> 7)));
             const float up = __uint_as_float(static_cast<uint32_t>(268 - e) << 23);
-            const float mys = __uint_as_float(static_cast<uint32_t>(e - 14) << 23) * p.scale_log2;
+            // a non-finite element makes the row's scores NaN, as its softmax is
+            const float mys = top >= 0x7f80u ? NAN : __uint_as_float(static_cast<uint32_t>(e - 14) << 23) * p.scale_log2;
 #pragma unroll
             for (int x = 0; x < 2; ++x) qscale[t][x] = __shfl_sync(0xffffffffu, mys, 4 * (2 * tig + x));
 #pragma unroll

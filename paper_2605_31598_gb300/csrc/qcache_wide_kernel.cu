@@ -637,9 +637,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const float up = __uint_as_float(static_cast<uint32_t>(min(254, 254 + kTop - e)) << 23);
                     qscale = __uint_as_float(static_cast<uint32_t>(e - kTop) << 23) * p.scale_log2;
                     uint8_t* sq = sQ + h * L::kQBytes;
+                    // a non-finite element makes the row's scores NaN, as its softmax is
+                    const bool bad = (top & 0xffffu) >= 0x7f80u || (top >> 16) >= 0x7f80u;
                     if constexpr (L::kDirect) {
-                        // a non-finite element makes the row's scores NaN, as its softmax is
-                        const bool bad = (top & 0xffffu) >= 0x7f80u || (top >> 16) >= 0x7f80u;
 #pragma unroll
                         for (int c = 0; c < D / 16; ++c) {
                             uint32_t hi4[4], lo4[4];
@@ -669,7 +669,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 make_uint4(lo4[0], lo4[1], lo4[2], lo4[3]);
                         }
                     } else {
-                        auto cv = [&](uint32_t w) { return pack_f16(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up); };
+                        auto cv = [&](uint32_t w) {
+                            return bad ? 0x7fff7fffu : pack_f16(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
+                        };
 #pragma unroll
                         for (int c = 0; c < D / 8; ++c)
                             *reinterpret_cast<uint4*>(sq + (c >> 3) * (kHalf * 128) + sw128_offset(row, c & 7)) =

@@ -112,3 +112,34 @@ def test_queries_with_an_outlier(d, rows, kind):
     assert ((lse[0, 0, :, 0].double() - z).abs() <= eps + 2.0 ** -20 * z.abs()).all()
     tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * eps[:, None, None]) * mag
     assert ((out.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("rows", [1, 30, 40])
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_that_are_not_finite(d, rows):
+    """A query with an infinity or a NaN has no softmax, whatever the keys: its output
+    and lse are NaN, and its neighbours' are within their own bounds."""
+    from paper_2605_31598_gb300 import QCache
+
+    held = 300
+    c = QCache(1, 1, 1, d, wide_capacity(rows), block_tokens=16)
+    k, v = noise((1, 1, held, 1, d), 1), noise((1, 1, held, 1, d), 2)
+    k[..., 3] = -k[..., 3].abs() - 0.5  # an infinity there makes every score -inf
+    k[..., 4] = k[..., 4].abs() + 0.5
+    zero = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    assert c.append(k, v, zero) == 0 and c.sync() == 0
+    q = noise((1, 1, rows, 2, d), 3)
+    start = zero + held - rows
+    kk, vv = dequantised(c, held)
+    want, size = definition(q, kk, vv, start)
+    total = torch.einsum("slnhd,slgjd->slnhj", q.double().abs(), kk.abs()).amax(-1)
+    tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * (2.0 ** -20 + d ** 0.5 * 2.0 ** -24 * total[..., None])) * size
+    inf = float("inf")
+    for place, value in ((3, inf), (3, -inf), (4, inf), (4, -inf), (9, inf), (9, float("nan"))):
+        bad = q.clone()
+        bad[0, 0, ::5, 1, place] = value
+        hit = torch.isnan(bad).any(-1) | torch.isinf(bad).any(-1)
+        out, z = torch.zeros_like(q), torch.zeros(q.shape[:4], device="cuda")
+        assert c.attend(bad, start, out, lse=z) == 0 and c.sync() == 0
+        assert torch.isnan(out[hit]).all() and torch.isnan(z[hit]).all(), (place, value)
+        assert ((out.double() - want).abs() <= tol)[~hit].all() and torch.isfinite(z[~hit]).all()
