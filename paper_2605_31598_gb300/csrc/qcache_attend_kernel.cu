@@ -14,9 +14,12 @@
 // in the workspace), always in the order of the keys, so results do not depend on
 // timing.
 //
-// Bound by HBM: a token of 28 layers, 28 query and 4 KV heads, 50,194 keys, D = 128:
-// 213.5 us, 6.74 TB/s.  One layer alone: 19.5 us, of which the 51 MB are 7.6 and the
-// start and the join the rest.
+// Bound by HBM for a token of D = 128: 28 layers, 28 query and 4 KV heads, 50,194 keys:
+// 212.6 us, 6.77 TB/s.  One layer alone: 19.7 us, of which the 51 MB are 7.6 and the
+// start and the join the rest.  Two tiles of 16 rows read the codes twice, as
+// they lie apart on the line: 28 rows of 28 layers over 12,548 keys 128 us, 106 for what
+// they read.  With D = 64 the warps' chain from codes to products bounds a token (two
+// warps to a scheduler, which issues in 40% of its cycles): 28 layers 149 us for 106.
 //
 // Inside a warp.  K and V codes of a step arrive as TMA copies (128-byte swizzle)
 // in the warp's ring, each stage behind an mbarrier.  Codes become fp16 in

@@ -20,8 +20,10 @@
 // Shared memory bounds the step: the products read 192 KB of operands for both
 // halves, and what the converters would move for K is another 48 KB (with it a step
 // took 4,150 cycles, now 3,620).
-// Measured: 1,000 tokens of 28 query and 4 KV heads behind 31,360 keys, D = 128: 412
-// us, 1.11 PFLOP/s, 58% of the bf16 rate.
+// Measured: 1,000 tokens of 28 query and 4 KV heads behind 31,360 keys, D = 128: 414
+// us, 1.10 PFLOP/s, 58% of the bf16 rate, where one key in twenty is three times the
+// others (rows set their references again); 374 us, 64%, on keys of one size.  D = 64:
+// 366 and 353 us.
 // TMEM: S0 | S1 | O0 | O1, 128 columns each.  Each half has an issuer that runs
 // PV(j), QK(j + 1), and the halves take turns: while one half's softmax works, the
 // tensor core has the other half's two products.  Q K^T into a half's scores

@@ -12,7 +12,7 @@
 // A CTA takes a token and forms its (cos, sin) pairs once, in shared memory.  A
 // thread stays at one place of the head rows, eight pairs (two 16-byte loads), with
 // their (cos, sin) in registers, and walks the heads; small CTAs, many to an SM, hide
-// one another's steps.  12,544 tokens of 72 heads of 128: 70.5 us, 6.56 TB/s (86 us
+// one another's steps.  12,544 tokens of 72 heads of 128: 70.8 us, 6.53 TB/s (86 us
 // reading the pairs from shared memory for every head, 78 with 256 threads, 95 and
 // more with several tokens to a CTA, whose registers leave too few CTAs).  Bound by
 // HBM for long inputs and by the launch for short ones (8 tokens: 2.2 us).
